@@ -335,6 +335,18 @@ int launch_rms_norm(const xema_rms_norm_args& a, cudaStream_t stream) {
   const uintptr_t rsize = a.resid_is_f32 ? 4 : 2, osize = a.out_is_e4m3 ? 1 : 2;
   auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
   if ((at(a.x) | at(a.gain)) & 1 || (at(a.resid) | at(a.resid_out)) % rsize || at(a.out) % osize || at(a.out_scale) & 3) return XEMA_EALIGN;
+  // A thread writes resid_out where it has read, and others may not have: over an operand only value for value.
+  auto rows_of = [&](const void* p, long long cols, long long ld, long long size) {
+    const long long pitch = ld * size;
+    return pitch < 0 ? Rows{static_cast<const char*>(p) + (p ? (a.rows - 1) * pitch : 0), a.rows, cols * size, -pitch} : Rows{p, a.rows, cols * size, pitch};
+  };
+  const Rows x = rows_of(a.x, a.D, a.ldx, 2), resid = rows_of(a.resid, a.D, a.ldr, rsize), gain = {a.gain, 1, 2LL * a.D, 0};
+  const Rows out = rows_of(a.out, a.D, a.ldo, osize), resid_out = rows_of(a.resid_out, a.D, a.ldro, rsize), factors = {a.out_scale, 1, 4LL * a.rows, 0};
+  auto in_place = [&](const Rows& in) { return in.p == resid_out.p && in.bytes == resid_out.bytes && (a.rows == 1 || in.pitch == resid_out.pitch); };
+  for (const Rows& in : {x, resid, gain})
+    if (rows_meet(out, in) || rows_meet(factors, in)) return XEMA_EINVAL;
+  if (rows_meet(resid_out, gain) || (!in_place(x) && rows_meet(resid_out, x)) || (!in_place(resid) && rows_meet(resid_out, resid))) return XEMA_EINVAL;
+  if (rows_meet(out, resid_out) || rows_meet(out, factors) || rows_meet(resid_out, factors)) return XEMA_EINVAL;
   // values that every row allows to be moved at once
   auto allows = [&](int e) {
     auto row = [&](const void* p, long long ld, uintptr_t size) {
