@@ -62,7 +62,8 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
   const Rows z = {a.z, 1, 6LL * a.rows * a.ffn, 0};
   for (const Rows& in : {x, wg, wu})
     if (rows_meet(h, in) || rows_meet(z, in)) return XEMA_EINVAL;
-  if (rows_meet(h, z)) return XEMA_EINVAL;
+  const Rows sx = {a.x_scale, 1, 4LL * a.rows, 0}, sg = {a.gate_scale, 1, 4LL * a.ffn, 0}, su = {a.up_scale, 1, 4LL * a.ffn, 0};
+  if (rows_meet(h, z) || rows_meet(h, sx) || rows_meet(h, sg) || rows_meet(h, su)) return XEMA_EINVAL;      // (no z with factors)
   const int step = 128 / elem;
   Params p = {};
   p.batch = 1;
