@@ -57,6 +57,8 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
   if ((a.rows > 1 && (a.ldx < a.width || a.ldh < a.ffn)) || a.ldw < a.width) return XEMA_EINVAL;
   if (!on16(a.x) || !on16(a.w_gate) || !on16(a.w_up) || !on16(a.h) || !on16(a.z)) return XEMA_EALIGN;
   if ((a.rows > 1 && (a.ldx % unit || a.ldh % 8)) || a.ldw % unit) return XEMA_EALIGN;
+  for (const float* f : {a.x_scale, a.gate_scale, a.up_scale})
+    if (reinterpret_cast<uintptr_t>(f) & 3) return XEMA_EALIGN;
   const Rows x = {a.x, a.rows, (long long)a.width * elem, a.ldx * elem}, h = {a.h, a.rows, a.ffn * 2LL, a.ldh * 2};
   const Rows wg = {a.w_gate, a.ffn, (long long)a.width * elem, a.ldw * elem}, wu = {a.w_up, a.ffn, (long long)a.width * elem, a.ldw * elem};
   const Rows z = {a.z, 1, 6LL * a.rows * a.ffn, 0};
