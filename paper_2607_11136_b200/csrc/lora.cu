@@ -114,7 +114,8 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   };
   const Rows out = span(a.out, a.N, a.ldo, a.out_batch_rows), work = {a.n_adapters > 0 ? a.work : nullptr, 1, (long long)lora_work_bytes(a.batch, a.rows, a.rank), 0};
   const Rows in[] = {span(a.x, a.K, a.ldx, a.x_batch_rows), {a.w, a.N, a.K * 2LL, a.ldw * 2}, {a.lora_a, 1, 2LL * a.n_adapters * a.rank * a.K, 0},
-                     {a.lora_b, 1, 2LL * a.n_adapters * a.rank * a.N, 0}};
+                     {a.lora_b, 1, 2LL * a.n_adapters * a.rank * a.N, 0}, {a.bias, 1, 2LL * a.N, 0}, {a.adapter, 1, 4LL * a.batch, 0},
+                     {a.n_adapters > 0 ? a.scale : nullptr, 1, 4LL * a.n_adapters, 0}};
   for (const Rows& i : in)
     if (rows_meet(out, i) || rows_meet(work, i)) return XEMA_EINVAL;
   if (rows_meet(out, work)) return XEMA_EINVAL;
