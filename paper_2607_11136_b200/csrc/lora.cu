@@ -64,6 +64,29 @@ __global__ void __launch_bounds__(kShrinkWarps * 32) shrink_kernel(const __nv_bf
   }
 }
 
+// The rows of `batch` requests, `step` rows from one to the next.
+struct Batches {
+  Rows one;
+  int batch;
+  long long step;
+  // all rows from the first to the last, those between the requests too
+  Rows all() const { return {one.p, (batch - 1) * (batch > 1 ? step : 0) + one.rows, one.bytes, one.pitch}; }
+};
+// Whether two of them share a byte.  With the same steps that is so for all pairs of requests if it is for one pair so far apart, and only
+// those count whose ranges meet: two or three where requests do not overlap.  Otherwise the rows between the requests count too.
+bool batches_meet(const Batches& a, const Batches& b) {
+  if (!rows_meet(a.all(), b.all())) return false;
+  if (a.batch == 1 || a.one.pitch != b.one.pitch || a.step != b.step || a.step < a.one.rows) return true;
+  const long long pitch = a.one.pitch * a.step, off = (long long)reinterpret_cast<uintptr_t>(b.one.p) - (long long)reinterpret_cast<uintptr_t>(a.one.p);
+  for (long long d = -off / pitch - 2; d <= -off / pitch + 2; ++d) {
+    if (d <= -a.batch || d >= a.batch) continue;
+    Rows shifted = b.one;
+    shifted.p = static_cast<const char*>(b.one.p) + d * pitch;
+    if (rows_meet(a.one, shifted)) return true;
+  }
+  return false;
+}
+
 // CTAs that share K of t, for a projection of `tiles` CTAs or (pair) pairs.  The projection starts on the SMs that t leaves free (a pair needs
 // both SMs of two neighbours) and has its first waves to go before it needs t: one CTA a tile where the projection fills the device for longer
 // than a wave, else as many as there is room for beside it, and (with enough of K to share) four where there is none and everything waits for
@@ -108,17 +131,14 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   if (a.ldw % 8 || (total > 1 && (a.ldx % 8 || a.ldo % 8))) return XEMA_EALIGN;
   if ((reinterpret_cast<uintptr_t>(a.adapter) | reinterpret_cast<uintptr_t>(a.scale)) & 3) return XEMA_EALIGN;
   if (reinterpret_cast<uintptr_t>(a.bias) & 1) return XEMA_EALIGN;
-  // all rows from the first to the last, those between the batch elements too
-  auto span = [&](const void* q, long long cols, long long ld, long long batch_rows) {
-    return Rows{q, (a.batch - 1) * (a.batch > 1 ? batch_rows : 0) + a.rows, cols * 2, ld * 2};
-  };
-  const Rows out = span(a.out, a.N, a.ldo, a.out_batch_rows), work = {a.n_adapters > 0 ? a.work : nullptr, 1, (long long)lora_work_bytes(a.batch, a.rows, a.rank), 0};
-  const Rows in[] = {span(a.x, a.K, a.ldx, a.x_batch_rows), {a.w, a.N, a.K * 2LL, a.ldw * 2}, {a.lora_a, 1, 2LL * a.n_adapters * a.rank * a.K, 0},
+  const Batches x = {{a.x, a.rows, a.K * 2LL, a.ldx * 2}, a.batch, a.x_batch_rows}, out = {{a.out, a.rows, a.N * 2LL, a.ldo * 2}, a.batch, a.out_batch_rows};
+  const Rows work = {a.n_adapters > 0 ? a.work : nullptr, 1, (long long)lora_work_bytes(a.batch, a.rows, a.rank), 0};
+  const Rows in[] = {{a.w, a.N, a.K * 2LL, a.ldw * 2}, {a.lora_a, 1, 2LL * a.n_adapters * a.rank * a.K, 0},
                      {a.lora_b, 1, 2LL * a.n_adapters * a.rank * a.N, 0}, {a.bias, 1, 2LL * a.N, 0}, {a.adapter, 1, 4LL * a.batch, 0},
                      {a.n_adapters > 0 ? a.scale : nullptr, 1, 4LL * a.n_adapters, 0}};
   for (const Rows& i : in)
-    if (rows_meet(out, i) || rows_meet(work, i)) return XEMA_EINVAL;
-  if (rows_meet(out, work)) return XEMA_EINVAL;
+    if (rows_meet(out.all(), i) || rows_meet(work, i)) return XEMA_EINVAL;
+  if (rows_meet(out.all(), work) || rows_meet(x.all(), work) || batches_meet(x, out)) return XEMA_EINVAL;
   Params p = {};
   p.batch = a.batch;
   p.rows = a.rows;
