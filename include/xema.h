@@ -450,7 +450,7 @@ int xema_op_attention(const void* q, int64_t ldq, int64_t q_batch_rows, const vo
 /* What a prompt encoder or a DiT block with a gated feed-forward runs besides attention: the norm with the
  * residual's addition, the gated feed-forward (with its gradients), and projections that all requests
  * of a batch share beside a low-rank adapter of each.  bf16 unless stated otherwise; sums, norms and
- * activations in fp32.  Sizes of zero rows are legal and launch nothing.  Results that share memory with an operand
+ * activations in fp32.  Sizes of zero rows are legal and launch nothing; the products' sizes go up to 2^31 - 256.  Results that share memory with an operand
  * or with one another are refused (XEMA_EINVAL) unless the operator says otherwise; rows side by side in one wider
  * matrix do not.  The operators may start while the launch before them in the stream ends, and wait for it before they
  * touch memory. */

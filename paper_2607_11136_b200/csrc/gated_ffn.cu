@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(256) gated_grad_kernel(const __nv_bfloat16* dh
 int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStream_t stream) {
   const int unit = a.is_e4m3 ? 16 : 8, elem = a.is_e4m3 ? 1 : 2;
   if (a.rows < 0 || a.width < unit || a.width % unit || a.ffn < 8 || a.ffn % 8) return XEMA_EINVAL;
+  if (a.rows > kMaxSize || a.width > kMaxSize || a.ffn > kMaxSize) return XEMA_EINVAL;
   if (a.activation != XEMA_ACT_SILU && a.activation != XEMA_ACT_GELU_TANH) return XEMA_EINVAL;
   if (a.rows == 0) return XEMA_OK;
   if (!a.x || !a.w_gate || !a.w_up || !a.h) return XEMA_EINVAL;
@@ -117,6 +118,7 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
 
 int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* status, cudaStream_t stream) {
   if (a.rows < 0 || a.width < 8 || a.width % 8 || a.ffn < 8 || a.ffn % 8) return XEMA_EINVAL;
+  if (a.rows > kMaxSize || a.width > kMaxSize || a.ffn > kMaxSize) return XEMA_EINVAL;
   if (a.activation != XEMA_ACT_SILU && a.activation != XEMA_ACT_GELU_TANH) return XEMA_EINVAL;
   if ((a.dw_gate == nullptr) != (a.dw_up == nullptr)) return XEMA_EINVAL;
   const bool want_w = a.dw_gate != nullptr, want_x = a.dx != nullptr;

@@ -119,6 +119,7 @@ unsigned long long lora_work_bytes(int batch, int rows, int rank) {
 
 int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stream) {
   if (a.batch < 0 || a.rows < 0 || a.K < 8 || a.K % 8 || a.N < 8 || a.N % 8 || a.n_adapters < 0) return XEMA_EINVAL;
+  if (a.batch > kMaxSize || a.rows > kMaxSize || a.K > kMaxSize || a.N > kMaxSize) return XEMA_EINVAL;
   if (a.rank < 8 || a.rank % 8 || a.rank > XEMA_LORA_MAX_RANK) return XEMA_EINVAL;
   if (a.batch == 0 || a.rows == 0) return XEMA_OK;
   if (!a.x || !a.w || !a.out || !a.adapter) return XEMA_EINVAL;

@@ -41,6 +41,7 @@ constexpr int kChunk = 32;                    // columns per epilogue step
 constexpr int kBufBytes = 2048;               // 32 rows x 32 columns of bf16
 constexpr int kRing = 2;                      // staging buffers per epilogue warp
 constexpr int kGroupM = 8;
+constexpr int kMaxSize = 0x7fffff00;          // of a dimension: a tile's last row and column, and one request more, stay within 32 bits
 
 constexpr int kStageArea = 196608;            // for the ring of stages
 constexpr int kMaxStages = 8;
