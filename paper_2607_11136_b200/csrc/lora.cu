@@ -37,9 +37,9 @@ __global__ void __launch_bounds__(kShrinkWarps * 32) shrink_kernel(const __nv_bf
   for (int g = warp * 32 + lane; g < K / 8; g += kShrinkWarps * 32) {
     uint4 av[RANKS], xv[TOK];
 #pragma unroll
-    for (int j = 0; j < RANKS; ++j) av[j] = __ldg(reinterpret_cast<const uint4*>(ar[j]) + g);
+    for (int j = 0; j < RANKS; ++j) av[j] = ld_u4(reinterpret_cast<const uint4*>(ar[j]) + g);
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) xv[i] = __ldg(reinterpret_cast<const uint4*>(xr[i]) + g);
+    for (int i = 0; i < TOK; ++i) xv[i] = ld_u4(reinterpret_cast<const uint4*>(xr[i]) + g);
 #pragma unroll
     for (int i = 0; i < TOK; ++i)
 #pragma unroll
