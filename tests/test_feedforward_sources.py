@@ -1,5 +1,8 @@
 """Rules of the feed-forward kernels that no result shows, checked on their sources."""
-from test_kernel_sources import _code
+import os
+import re
+
+from test_kernel_sources import CSRC, _code, _headers
 
 FILES = ("rms_norm.cu", "gated_ffn.cu", "lora.cu", "tile_gemm.cuh", "skinny_gemm.cuh")
 
@@ -10,3 +13,62 @@ def test_no_read_only_loads_in_chained_kernels():
     for name in FILES:
         code = _code(name)
         assert "__ldg" not in code and "ld.global.nc" not in code and "__restrict__" not in code, name
+
+
+# What a wait for earlier launches stands under, with the reason why nothing of theirs is touched without it.  `late`: a projection right behind
+# the kernel that makes t, which lets it start only after its own wait has returned -- so x, W, bias, adapters and the requests' indices are there, and only
+# t and the memory of the results have to be waited for.
+WAITS = {
+    "tile_gemm.cuh": {
+        "if (!late)": 1,                                        # all threads, before anything is read
+        "if (late && s0 + KSUB > p.k_main) ;": 1,               # producer: ahead of the first step that reads t
+        "if (late)": 1,                                         # epilogue: ahead of the first store
+    },
+    "skinny_gemm.cuh": {
+        "if constexpr (SHRINK)": 1,                             # t itself: all threads, before the adapter's index is read
+        "if (!late)": 1,                                        # the others: all threads, before anything is read
+        "if (late) ;": 1,                                       # producer: ahead of the first load of t
+        "if (late)": 1,                                         # epilogue: ahead of t (single tokens) and of the closing barrier, behind which results are written
+    },
+}
+
+
+def test_every_conditional_wait_of_the_product_headers_is_listed():
+    for name in sorted(f for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))):
+        if name == "sm100.cuh":
+            continue                                            # (where it is defined)
+        code, under = _code(name), {}
+        for m in re.finditer(r"([^;{}]*)\bgrid_dep_wait\(\)", code):
+            before = " ".join(m.group(1).split())
+            head = before + " ;" if before else _headers(code, m.start(1))[0]
+            under[head] = under.get(head, 0) + 1
+        assert under == WAITS.get(name, {}), name
+
+
+def test_the_next_launch_may_start_only_behind_a_wait_and_with_tensor_memory_in_hand():
+    launches = 0
+    for name in FILES:
+        code = _code(name)
+        for m in re.finditer(r"\bgrid_dep_launch\(\)", code):
+            launches += 1
+            statements = [" ".join(t.split()) for t in re.split(r"[;{}]", code[:m.start()])]
+            assert statements[-1] in ("", "if (threadIdx.x == 0)", "if (et == 0)") and statements[-2] == "grid_dep_wait()", (name, statements[-2:])
+            if name.endswith(".cuh"):
+                body = code[code.rindex("extern __shared__", 0, m.start()):m.start()]
+                assert "tmem_alloc(tmem_slot" in body and "__syncthreads()" in body[body.index("tmem_alloc(tmem_slot"):], name
+    assert launches == 8
+
+
+def test_what_waits_late_reads_nothing_of_t_before():
+    tile, few = _code("tile_gemm.cuh"), _code("skinny_gemm.cuh")
+    # tiles: t's map is read at one place, for steps behind K's own
+    assert tile.count("maps.a2") == 1 and "if (s < p.k_main)" in tile[:tile.index("maps.a2")]
+    # few tokens: t's map and pointer are read behind the producer's and the epilogue's waits
+    load = few.index("&maps.t, &full")
+    assert "if (late) grid_dep_wait();" in few[few.index("if (warp == 0) {"):load]
+    use = few.index("p.t +")
+    epilogue = few[few.index("const int quad = warp & 3"):]
+    assert epilogue.index("grid_dep_wait()") < epilogue.index("p.t +") and few.count("p.t +") == 1 and use > load
+    # nothing is stored before the epilogue has waited: stores stand behind a barrier of all threads
+    assert few.index("store_bf16x8(p.") > few.rindex("__syncthreads()")
+    assert tile.count("tma_store_3d(") == 1 and tile.index("if (late) {") < tile.index("tma_store_3d(")
