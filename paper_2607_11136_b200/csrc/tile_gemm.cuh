@@ -422,11 +422,14 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&tmem_empty[acc]), 0));
-        else mbar_arrive(&tmem_empty[acc]);
+      // only the tile after the next asks for this accumulator
+      if (tile + 2 * n_workers < total_tiles) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&tmem_empty[acc]), 0));
+          else mbar_arrive(&tmem_empty[acc]);
+        }
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }

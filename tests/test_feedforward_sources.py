@@ -72,3 +72,13 @@ def test_what_waits_late_reads_nothing_of_t_before():
     # nothing is stored before the epilogue has waited: stores stand behind a barrier of all threads
     assert few.index("store_bf16x8(p.") > few.rindex("__syncthreads()")
     assert tile.count("tma_store_3d(") == 1 and tile.index("if (late) {") < tile.index("tma_store_3d(")
+
+
+def test_an_accumulator_is_released_only_where_a_later_tile_asks_for_it():
+    """The odd CTA of a pair releases by an arrival on the even CTA's barrier: one that nobody waits for would be under way while the pair leaves."""
+    tile = _code("tile_gemm.cuh")
+    release = tile.index("mbar_arrive_cluster(mapa_shared(smem_u32(&tmem_empty[acc]), 0))")
+    heads = _headers(tile, release)
+    assert any(h.startswith("if (") and "tile + 2 * n_workers < total_tiles" in h for h in heads), heads
+    # two accumulators in turn: the tile after the next is the one that asks
+    assert "mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1" in tile and tile.count("if (++acc == 2)") == 2
