@@ -154,6 +154,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
   if (!late) {
     grid_dep_wait();
     if (threadIdx.x == 0) grid_dep_launch();
+    __syncwarp();
   }
 
   // kPacked: lane j has slot j's adapter
@@ -283,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
     if (late) {
       grid_dep_wait();
       if (et == 0) grid_dep_launch();
+      __syncwarp();
     }
     if constexpr (LORA) {
       for (int i = first + et; i < last; i += 128) {
@@ -315,6 +317,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
     if constexpr (PACKED) {
       if (et < p.slots && b0 + et < p.batch && p.adapter[b0 + et] >= p.n_adapters && p.status) atomicExch(p.status, XEMA_DEVICE_STATUS_ADAPTER);
     }
+    __syncwarp();              // (the lanes' last groups differ; the loads from TMEM want whole warps)
     const bool ok = aligned && mbar_wait_warp(done, 0, abort_flag);
     tc_fence_after();
     if (ok) {

@@ -192,6 +192,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
   if (!late) {
     grid_dep_wait();
     if (threadIdx.x == 0) grid_dep_launch();
+    __syncwarp();
   }
 
   if (warp == 0) {
@@ -335,6 +336,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
     if (late) {
       grid_dep_wait();
       if (et == 0) grid_dep_launch();
+      __syncwarp();
     }
     // 32 columns of the warp's rows, 16 bits each, on their way to the map's (x, y, z)
     auto send_raw = [&](const uint32_t (&w)[kChunk / 2], const CUtensorMap& m, int x, int y, int z) {
@@ -350,6 +352,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
         tma_store_3d(&m, buf, x, y, z);
         bulk_commit();
       }
+      __syncwarp();          // (the next load from TMEM, or vote, wants whole warps)
       ++used;
     };
     auto send = [&](const float (&v)[kChunk], const CUtensorMap& m, int x, int y, int z) {
@@ -430,6 +433,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
           if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&tmem_empty[acc]), 0));
           else mbar_arrive(&tmem_empty[acc]);
         }
+        __syncwarp();
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }

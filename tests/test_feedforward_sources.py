@@ -82,3 +82,45 @@ def test_an_accumulator_is_released_only_where_a_later_tile_asks_for_it():
     assert any(h.startswith("if (") and "tile + 2 * n_workers < total_tiles" in h for h in heads), heads
     # two accumulators in turn: the tile after the next is the one that asks
     assert "mbar_wait_cluster(&tmem_empty[acc], acc_phase ^ 1" in tile and tile.count("if (++acc == 2)") == 2
+
+
+def _after(code, at):
+    """The statement behind the one (or the block) that begins at `at`, which is an if."""
+    depth, i = 0, code.index("(", at)
+    while True:                                   # the condition
+        depth += {"(": 1, ")": -1}.get(code[i], 0)
+        i += 1
+        if depth == 0:
+            break
+    while code[i].isspace():
+        i += 1
+    if code[i] == "{":
+        depth = 0
+        while True:
+            depth += {"{": 1, "}": -1}.get(code[i], 0)
+            i += 1
+            if depth == 0:
+                break
+    else:
+        i = code.index(";", i) + 1
+    return " ".join(code[i:].split())
+
+
+def test_whole_warps_meet_behind_what_one_lane_does():
+    """tcgen05.ld, elect.sync, barrier.cluster and bar.red want all lanes of a warp at once: behind a branch that a single lane takes,
+    __syncwarp() is the next thing that happens."""
+    found = 0
+    for name in ("tile_gemm.cuh", "skinny_gemm.cuh"):
+        code = _code(name)
+        code = code[:code.index("struct Shape {" if name == "tile_gemm.cuh" else "int launch_clusters(")]
+        for m in re.finditer(r"\bif \((lane == 0|et == 0|threadIdx\.x == 0|(ok && )?elect_one\(\))\)", code):
+            if "mbar_init" in code[m.end():m.end() + 120]:
+                continue                          # the barriers' setup: __syncthreads() stands behind it, and warp 1's own work between
+            found += 1
+            rest = _after(code, m.start())
+            assert re.match(r"(else mbar_arrive\(&tmem_empty\[acc\]\); |\+\+used; |\} )*__syncwarp\(\);", rest), (name, m.group(), rest[:80])
+    assert found == 17
+    # loops whose lanes leave at different rounds, ahead of a wait that a warp polls together
+    few = _code("skinny_gemm.cuh")
+    ahead = few[:few.index("const bool ok = aligned && mbar_wait_warp(done")]
+    assert ahead.rstrip().endswith("__syncwarp();")
