@@ -215,6 +215,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
       }
     }
     if (!ok && aligned) {
+      report_timeout(p.status);
       // gave up: copies under way must land before the CTA leaves
       if (lane == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -278,6 +279,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
     }
     if (ok && elect_one()) mma_commit(done);
     __syncwarp();
+    if (!ok) report_timeout(p.status);
   } else {
     // ---------------- epilogue ----------------
     const int quad = warp & 3, et = threadIdx.x - 64;
@@ -319,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
     }
     __syncwarp();              // (the lanes' last groups differ; the loads from TMEM want whole warps)
     const bool ok = aligned && mbar_wait_warp(done, 0, abort_flag);
+    if (!ok) report_timeout(p.status);
     tc_fence_after();
     if (ok) {
       // all MMAs are done, so the ring is free: sums as [token][row] (fp32), row = gate features, then up
@@ -415,7 +418,6 @@ __global__ void __launch_bounds__(kThreads, 2) skinny_kernel(const __grid_consta
     cluster_arrive();          // nobody leaves while its sums may still be read
     cluster_wait();
   }
-  if (threadIdx.x == 0 && *abort_flag && p.status) atomicExch(p.status, STATUS_TIMEOUT_MBARRIER);
 }
 
 // The instance for a tile of `nt` columns.

@@ -157,6 +157,11 @@ __device__ __forceinline__ void mbar_wait_sticky(uint64_t* bar, uint32_t parity,
   if (!mbar_test(bar, parity)) ok = mbar_wait_warp(bar, parity, abort_flag) && ok;
 }
 
+// A wait gave up: into the caller's status word, by one lane of the warp that waited.
+__device__ __forceinline__ void report_timeout(unsigned int* status) {
+  if (status && (threadIdx.x & 31) == 0) atomicExch(status, STATUS_TIMEOUT_MBARRIER);
+}
+
 // ---- programmatic dependent launch -----------------------------------------------------------
 // A kernel that launch_kernel chains may start while the launch before it still runs.  It has to
 // call grid_dep_wait() in every thread that reads what earlier launches wrote (or overwrites what

@@ -264,6 +264,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
       }
     }
     if (!ok) {
+      report_timeout(p.status);
       // Gave up: copies under way must land before a CTA leaves.  All of a pair complete on the even CTA's barriers; the closing
       // cluster barrier keeps the peer until then, a short settling time covers a stage that only one of them still asked for.
       if (rank == 0 && lane == 0) {
@@ -325,6 +326,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
         __syncwarp();
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
+      if (!ok) report_timeout(p.status);
     }
   } else {
     // ---------------- epilogue (pair: each CTA its own 128 rows) ----------------
@@ -437,6 +439,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
+    if (!ok) report_timeout(p.status);
     if (lane == 0) bulk_wait<0>();       // this warp's stores are complete
     __syncwarp();
     if (FORM == Form::kLinear && blockIdx.x == 0 && p.adapter && p.status) {
@@ -457,7 +460,7 @@ __device__ __forceinline__ void body(const Maps& maps, const Params& p) {
     if (PAIR) tmem_dealloc_pair(tmem_base, 2 * ACC_COLS);
     else tmem_dealloc(tmem_base, 2 * ACC_COLS);
   }
-  if (threadIdx.x == 0 && *abort_flag && p.status) atomicExch(p.status, STATUS_TIMEOUT_MBARRIER);
+  if (threadIdx.x == 0 && !aligned) report_timeout(p.status);
 }
 
 template <Form FORM, bool F8>

@@ -124,3 +124,19 @@ def test_whole_warps_meet_behind_what_one_lane_does():
     few = _code("skinny_gemm.cuh")
     ahead = few[:few.index("const bool ok = aligned && mbar_wait_warp(done")]
     assert ahead.rstrip().endswith("__syncwarp();")
+
+
+def test_a_wait_that_gives_up_is_reported_at_once():
+    """... and not behind the closing barriers, which a CTA whose peer has stopped never passes: once in each role, ahead of anything that could wait."""
+    for name, closing in (("tile_gemm.cuh", "// Neither CTA"), ("skinny_gemm.cuh", "// TMEM goes back")):
+        raw = open(os.path.join(CSRC, name)).read()
+        roles = raw[raw.index("TMA producer -"):raw.index(closing)]
+        parts = re.split(r"// -+ (?:MMA issuer|epilogue)[^\n]*-", roles)
+        assert len(parts) == 3
+        for part in parts:
+            code = re.sub(r"//[^\n]*", "", part)
+            assert code.count("report_timeout(p.status)") == 1, name
+            at = code.index("report_timeout(p.status)")
+            assert "mbar_wait_slow" not in code[:at] and "bulk_wait<0>" not in code[:at], name
+    helper = _code("sm100.cuh")
+    assert "atomicExch(status, STATUS_TIMEOUT_MBARRIER)" in helper[helper.index("void report_timeout("):]
