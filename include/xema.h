@@ -457,7 +457,7 @@ int xema_op_attention(const void* q, int64_t ldq, int64_t q_batch_rows, const vo
 
 /* v = x + resid (fp32);  out = v / sqrt(mean(v^2) + eps) * gain, per row;  resid_out = v.
  * out in bf16, or in e4m3 with one factor per row: out_scale = max|.| / 448 (at least FLT_MIN, so that a
- * row of zeros stays one) and out = (.) / out_scale rounded to nearest.  A NaN, or an infinity in v, makes its row NaN; finite rows
+ * row of zeros stays one) and out = (.) / out_scale in fp32, rounded to nearest.  A NaN, or an infinity in v, makes its row NaN; finite rows
  * may be as large as v's type allows.  (mean(v^2) + eps is an fp32 number: below 2^-126, as only a tiny eps leaves it, it is lost.)
  * Any width up to XEMA_RMS_NORM_MAX_D and any strides; rows whose pointers lie on 16-byte boundaries, with
  * strides and D a multiple of 8, are read and written 16 bytes at a time.  x and resid may share memory, and resid_out may be
