@@ -2,6 +2,7 @@
 // functions are handed over as addresses by the package's loader (no link between this module and the library).  In C++ because a
 // small call's time is the host's: the same steps in Python take 9 to 14 us beside a kernel of 2 to 5.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -33,10 +34,13 @@ void need(bool ok, const char* what) {
 }
 bool given(PyObject* o) { return o && o != Py_None; }
 
-// The tensor behind `o`, on device `index` (or any CUDA device: -1), of this type and rank.
-const Tensor& tensor(PyObject* o, const char* name, at::ScalarType type, int64_t rank, int index) {
+// The tensor behind `o`, on device `index` (or any CUDA device: -1), of this type and rank.  Operators whose results would have to carry
+// a gradient on (`recorded`) take none that requires one while gradients are on: the loss would run backward without them.
+const Tensor& tensor(PyObject* o, const char* name, at::ScalarType type, int64_t rank, int index, bool recorded = true) {
   if (!THPVariable_Check(o)) refuse(std::string(name) + ": want a tensor");
   const Tensor& t = THPVariable_Unpack(o);
+  if (recorded && t.requires_grad() && c10::GradMode::is_enabled())
+    refuse(std::string(name) + ": requires a gradient, which the result would not carry on: call under torch.no_grad() (gated_ffn_backward has gated_ffn's gradients)");
   if (!t.is_cuda() || (index >= 0 && t.get_device() != index))
     refuse(std::string(name) + (index >= 0 ? ": want it on the device of the other tensors" : ": want tensors on a CUDA device (there is no CPU fallback)"));
   if (t.scalar_type() != type) refuse(std::string(name) + ": want " + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
@@ -153,8 +157,8 @@ struct Weights {
   const void *gate, *up;
   int64_t ffn, ld;
 };
-Weights weights(PyObject* g, PyObject* u, at::ScalarType type, int64_t width, int index) {
-  const Tensor &gate = tensor(g, "w_gate", type, 2, index), &up = tensor(u, "w_up", type, 2, index);
+Weights weights(PyObject* g, PyObject* u, at::ScalarType type, int64_t width, int index, bool recorded = true) {
+  const Tensor &gate = tensor(g, "w_gate", type, 2, index, recorded), &up = tensor(u, "w_up", type, 2, index, recorded);
   sized(gate, "w_gate", {gate.size(0), width});
   sized(up, "w_up", {gate.size(0), width});
   const bool one = gate.size(0) == 1;
@@ -223,13 +227,13 @@ PyObject* gated_ffn(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyObject* gated_ffn_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   argc(n, 10);
-  const Tensor& x = tensor(v[1], "x", kBf16, 2, -1);
+  const Tensor& x = tensor(v[1], "x", kBf16, 2, -1, false);
   const int index = x.get_device();
   const int64_t rows = x.size(0), width = x.size(1);
-  const Weights w = weights(v[2], v[3], kBf16, width, index);
-  const Tensor& dh = tensor(v[0], "dh", kBf16, 2, index);
+  const Weights w = weights(v[2], v[3], kBf16, width, index, false);
+  const Tensor& dh = tensor(v[0], "dh", kBf16, 2, index, false);
   sized(dh, "dh", {rows, w.ffn});
-  const Tensor& saved = tensor(v[4], "saved", kI16, 3, index);
+  const Tensor& saved = tensor(v[4], "saved", kI16, 3, index, false);
   sized(saved, "saved", {3, rows, w.ffn});
   need(saved.is_contiguous(), "saved: want it as gated_ffn gave it");
   xema_gated_ffn_grad_args a = {};

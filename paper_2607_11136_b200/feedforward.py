@@ -9,6 +9,9 @@ Everything runs on the current stream of the tensors' device, without synchronis
 torch's allocator unless the caller gives the results.  Last dimensions are contiguous, other strides are free.  Arguments that
 the operators do not take raise ValueError or XemaError before anything is launched; what a kernel finds out later (an adapter
 index beyond the adapters, a wait that ran out) is raised by `check`.
+
+The functions are not recorded by autograd: while gradients are on, operands that require one are refused.  In a training program they stand in a
+torch.autograd.Function, or under torch.no_grad(), and gated_ffn_backward is the gradient of gated_ffn.
 """
 from __future__ import annotations
 
