@@ -59,8 +59,11 @@ def _status_of(t) -> int:
 
 
 def check(device=None) -> None:
-    """Waits for the device and raises XemaError if a kernel of this module reported a failure since the last check."""
-    index = _current_device() if device is None else torch.device(device).index or 0
+    """Waits for the device (the current one, unless given) and raises XemaError if a kernel of this module reported a failure since
+    the last check."""
+    index = None if device is None else torch.device(device).index
+    if index is None:
+        index = _current_device()
     torch.cuda.synchronize(index)
     if index not in _status:
         return
