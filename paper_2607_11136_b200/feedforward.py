@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 
 import torch
 
@@ -26,6 +27,7 @@ from .session import _current_device
 _ACTIVATIONS = {"silu": xb.ACT_SILU, "gelu_tanh": xb.ACT_GELU_TANH}
 _TYPES = {torch.bfloat16: False, torch.float8_e4m3fn: True}
 _status = {}
+_status_lock = threading.Lock()
 _module = None
 
 
@@ -53,9 +55,11 @@ def _status_of(t) -> int:
         raise ValueError("want tensors on a CUDA device (there is no CPU fallback)")
     if torch.cuda.is_current_stream_capturing():
         raise RuntimeError("the first call on a device makes its status word: make one before the capture begins")
-    word = torch.zeros(1, dtype=torch.int32, device="cuda:%d" % index)
-    _status[index] = (word, word.data_ptr())
-    return word.data_ptr()
+    with _status_lock:
+        if index not in _status:
+            word = torch.zeros(1, dtype=torch.int32, device="cuda:%d" % index)
+            _status[index] = (word, word.data_ptr())
+        return _status[index][1]
 
 
 def check(device=None) -> None:

@@ -27,3 +27,38 @@ def test_check_without_an_index_looks_at_the_current_device(monkeypatch):
     with pytest.raises(Exception, match="adapter"):
         ff.check("cuda")
     assert word.item() == 0
+
+
+class _OnDevice0(torch.Tensor):
+    def get_device(self):
+        return 0
+
+
+@pytest.fixture
+def no_device(monkeypatch):
+    """What making a status word calls of torch, on the CPU and slowly; the words that were made."""
+    made, zeros = [], torch.zeros
+
+    def slow_zeros(*size, **kw):
+        time.sleep(0.05)
+        kw.pop("device")
+        made.append(zeros(*size, **kw))
+        return made[-1]
+
+    monkeypatch.setattr(ff, "_status", {})
+    monkeypatch.setattr(torch, "zeros", slow_zeros)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), {"synchronize": lambda self: None})())
+    return made
+
+
+def test_threads_get_the_same_status_word(no_device):
+    """One word a device: of two, one would be freed while kernels hold its address."""
+    t = torch.empty(1).as_subclass(_OnDevice0)
+    got = []
+    threads = [threading.Thread(target=lambda: got.append(ff._status_of(t))) for _ in range(8)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert len(no_device) == 1 and got == [no_device[0].data_ptr()] * 8
