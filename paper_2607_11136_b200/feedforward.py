@@ -58,6 +58,7 @@ def _status_of(t) -> int:
     with _status_lock:
         if index not in _status:
             word = torch.zeros(1, dtype=torch.int32, device="cuda:%d" % index)
+            torch.cuda.current_stream(index).synchronize()      # (other streams may be the first to use it)
             _status[index] = (word, word.data_ptr())
         return _status[index][1]
 

@@ -62,3 +62,12 @@ def test_threads_get_the_same_status_word(no_device):
     for th in threads:
         th.join()
     assert len(no_device) == 1 and got == [no_device[0].data_ptr()] * 8
+
+
+def test_a_status_word_is_zero_before_its_address_is_given_out(no_device, monkeypatch):
+    """Kernels on other streams than the one that fills it would write into memory that is filled later."""
+    seen = []
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda device=None: type("Stream", (), {"synchronize": lambda self: seen.append((device, len(no_device), dict(ff._status)))})())
+    ff._status_of(torch.empty(1).as_subclass(_OnDevice0))
+    assert seen == [(0, 1, {})]
