@@ -55,7 +55,7 @@ def _status_of(t) -> int:
         raise ValueError("want tensors on a CUDA device (there is no CPU fallback)")
     if torch.cuda.is_current_stream_capturing():
         raise RuntimeError("the first call on a device makes its status word: make one before the capture begins")
-    with _status_lock:
+    with _status_lock, torch.inference_mode(False):       # (a word made in that mode could not be cleared outside)
         if index not in _status:
             word = torch.zeros(1, dtype=torch.int32, device="cuda:%d" % index)
             torch.cuda.current_stream(index).synchronize()      # (other streams may be the first to use it)

@@ -71,3 +71,13 @@ def test_a_status_word_is_zero_before_its_address_is_given_out(no_device, monkey
                         lambda device=None: type("Stream", (), {"synchronize": lambda self: seen.append((device, len(no_device), dict(ff._status)))})())
     ff._status_of(torch.empty(1).as_subclass(_OnDevice0))
     assert seen == [(0, 1, {})]
+
+
+def test_a_status_word_made_in_inference_mode_can_be_cleared_outside(no_device, monkeypatch):
+    with torch.inference_mode():
+        ff._status_of(torch.empty(1).as_subclass(_OnDevice0))
+    no_device[0][0] = 0x54310002
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: None)
+    with pytest.raises(Exception, match="adapter"):
+        ff.check(0)
+    ff.check(0)
