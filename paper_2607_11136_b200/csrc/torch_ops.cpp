@@ -80,6 +80,11 @@ PyObject* answer(int rc, const Tensor (&t)[N]) {
 void argc(Py_ssize_t n, Py_ssize_t want) {
   if (n != want) refuse("wrong number of arguments");
 }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();      // (the exception that is set)
+  return v;
+}
 double number(PyObject* o, const char* name) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) {
@@ -124,7 +129,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
   sized(gain, "gain", {D});
   a.gain = address(gain);
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)index);
-  a.out_is_e4m3 = PyObject_IsTrue(v[4]);
+  a.out_is_e4m3 = truth(v[4]);
   Tensor t[3];
   if (given(v[5])) {
     t[0] = tensor(v[5], "out", a.out_is_e4m3 ? kE4m3 : kBf16, 2, index);
@@ -188,7 +193,7 @@ PyObject* gated_ffn(PyObject*, PyObject* const* v, Py_ssize_t n) {
   a.ffn = i32(w.ffn, "w_gate");
   a.activation = (int)PyLong_AsLong(v[3]);
   a.is_e4m3 = e4m3;
-  const bool save = PyObject_IsTrue(v[8]);
+  const bool save = truth(v[8]);
   if (e4m3) {
     need(!save, "save: gradients are for bf16 operands");
     const Tensor &sx = tensor(v[4], "x_scale", kF32, 1, index), &sg = tensor(v[5], "gate_scale", kF32, 1, index),
@@ -250,15 +255,15 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
   a.ffn = i32(w.ffn, "w_gate");
   a.activation = (int)PyLong_AsLong(v[5]);
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)index);
-  const Tensor work = PyObject_IsTrue(v[8]) ? saved : fresh({2, rows, w.ffn}, kBf16, x);
+  const Tensor work = truth(v[8]) ? saved : fresh({2, rows, w.ffn}, kBf16, x);
   a.work = address(work);
   Tensor t[3];
-  if (PyObject_IsTrue(v[6])) {
+  if (truth(v[6])) {
     t[0] = fresh({rows, width}, kBf16, x);
     a.dx = address(t[0]);
     a.lddx = width;
   }
-  if (PyObject_IsTrue(v[7])) {
+  if (truth(v[7])) {
     t[1] = fresh({w.ffn, width}, kBf16, x);
     t[2] = fresh({w.ffn, width}, kBf16, x);
     a.dw_gate = address(t[1]);
