@@ -8,6 +8,7 @@ import subprocess
 import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
+from importlib import metadata, util
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -46,6 +47,18 @@ def _torch_ops_command(source: str) -> list:
             + ["-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python"])
 
 
+def _torch_stamp() -> str:
+    """The torch and the Python that the module for torch tensors is built against."""
+    return "torch %s at %s, Python %s\n" % (metadata.version("torch"), util.find_spec("torch").origin, sys.version)
+
+
+def _read(path: str) -> str:
+    if not os.path.exists(path):
+        return ""
+    with open(path) as f:
+        return f.read()
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles every source for sm_100a and links libxema.so and _torch_ops.so.  Returns the library path."""
     os.makedirs(OBJ, exist_ok=True)
@@ -64,7 +77,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
     torch_ops = os.path.join(CSRC, "torch_ops.cpp")
     links = len(jobs)
-    if force or _stale(TORCH_OPS, [torch_ops, headers[-1]]):
+    stamp = os.path.join(OBJ, "torch_ops.stamp")
+    if force or _stale(TORCH_OPS, [torch_ops, headers[-1]]) or _read(stamp) != _torch_stamp():
         jobs.append(_torch_ops_command(torch_ops))
 
     def run(cmd):
@@ -77,6 +91,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         for out in ex.map(run, jobs):
             if verbose and out:
                 print(out, file=sys.stderr)
+    if len(jobs) > links:
+        with open(stamp, "w") as f:
+            f.write(_torch_stamp())
     if links or force or _stale(LIB, objs):
         run([nvcc, "-shared", "-o", LIB] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"])
     return LIB

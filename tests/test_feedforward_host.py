@@ -81,3 +81,33 @@ def test_a_status_word_made_in_inference_mode_can_be_cleared_outside(no_device, 
     with pytest.raises(Exception, match="adapter"):
         ff.check(0)
     ff.check(0)
+
+
+def test_the_torch_module_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
+    """Sources that did not change are no reason to keep a module that was built against another torch or Python."""
+    from paper_2607_11136_b200 import build as b
+    commands = []
+    monkeypatch.setattr(b, "OBJ", str(tmp_path))
+    monkeypatch.setattr(b, "TORCH_OPS", str(tmp_path / "_torch_ops.so"))
+    monkeypatch.setattr(b, "LIB", str(tmp_path / "libxema.so"))
+    monkeypatch.setattr(b, "SOURCES", [])
+    monkeypatch.setattr(b, "_torch_ops_command", lambda source: ["torch-ops", source])
+
+    def run(cmd, **kw):
+        commands.append(cmd[0])
+        open(b.TORCH_OPS if cmd[0] == "torch-ops" else b.LIB, "w").close()
+        return type("Result", (), {"returncode": 0, "stdout": "", "stderr": ""})()
+
+    monkeypatch.setattr(b.subprocess, "run", run)
+    b.build()
+    assert commands.count("torch-ops") == 1
+    b.build()
+    assert commands.count("torch-ops") == 1
+    version = b.metadata.version
+    monkeypatch.setattr(b.metadata, "version", lambda name: version(name) + ".other")
+    b.build()
+    b.build()
+    assert commands.count("torch-ops") == 2
+    monkeypatch.setattr(b.sys, "version", "another Python")
+    b.build()
+    assert commands.count("torch-ops") == 3
