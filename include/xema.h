@@ -550,6 +550,22 @@ typedef struct xema_lora_args {
 int xema_op_lora(const xema_lora_args* args, void* status_dev, void* stream);
 uint64_t xema_lora_work_bytes(int32_t batch, int32_t rows, int32_t rank);
 
+/* For tests: the products above in a kernel and shape of the caller's choice instead of the one that is estimated to be fastest (XEMA_EINVAL
+ * where the product cannot run in it).  Results are within the same rounding errors in all, not the same bits.
+ *   XEMA_FF_TILES    columns of the product per tile: pair 1: 256 rows over two SMs, 128 to 256 columns in steps of 32 (gated: 64);
+ *                    pair 0: 128 x 128 on one
+ *   XEMA_FF_FEW      few tokens (at most 1024; with adapters 512 a request): share (1, 2, 4) CTAs along K, features (a multiple of 8, at most 128; dx: 64 or
+ *                    128) a CTA; 0: as estimated
+ *   XEMA_FF_SINGLE   adapters, one row a request: the same for single tokens
+ * share_t: CTAs along K of the launch that makes x lora_a^T, where that is one of tiles; 0: as estimated. */
+enum { XEMA_FF_TILES = 1, XEMA_FF_FEW = 2, XEMA_FF_SINGLE = 3 };
+typedef struct xema_ff_shape {
+  int32_t kernel, pair, columns, share, features;
+} xema_ff_shape;
+int xema_op_gated_ffn_in(const xema_gated_ffn_args* args, const xema_ff_shape* shape, void* status_dev, void* stream);
+int xema_op_gated_ffn_grad_in(const xema_gated_ffn_grad_args* args, const xema_ff_shape* dx, const xema_ff_shape* dw, void* status_dev, void* stream);
+int xema_op_lora_in(const xema_lora_args* args, const xema_ff_shape* shape, int32_t share_t, void* status_dev, void* stream);
+
 /* ---- allocator plug-in ------------------------------------------------------------------ */
 /* The paper's run-time mechanism for code that is not this library's own kernels (section
  * "Static memory runtime"; implementation: PyTorch's CUDAPluggableAllocator): a framework hands

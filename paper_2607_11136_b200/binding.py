@@ -18,6 +18,7 @@ XEMA_OK, XEMA_EINVAL, XEMA_ENOSPC, XEMA_EBUDGET = 0, -1, -2, -3
 XEMA_EALIGN, XEMA_ECUDA, XEMA_ETIMEOUT, XEMA_ESTATE = -4, -5, -6, -7
 ACT_SILU, ACT_GELU_TANH = 0, 1
 RMS_NORM_MAX_D, LORA_MAX_RANK = 65536, 128
+FF_TILES, FF_FEW, FF_SINGLE = 1, 2, 3
 EPI_BIAS, EPI_BIAS_GELU, EPI_GATE_RES_F32, EPI_GATE_RES_BF16, EPI_BIAS_NORM_ROPE = 0, 1, 2, 3, 4
 
 EXPORTS = (
@@ -29,7 +30,7 @@ EXPORTS = (
     "xema_block_forward_static",
     "xema_shard_rows", "xema_trace_sharded", "xema_plan_create_sharded", "xema_plan_shard", "xema_plan_gather_point", "xema_plan_create_guarded", "xema_plan_guard_bytes",
     "xema_plan_launch_count", "xema_plan_forward_launches", "xema_forward_host", "xema_forward_prefix", "xema_forward_range", "xema_plan_op", "xema_op_mod", "xema_op_ln_modulate",
-    "xema_op_rmsnorm_rope", "xema_op_gemm", "xema_gemm_tile", "xema_op_gemm_in_tile", "xema_op_attention", "xema_op_rms_norm", "xema_op_gated_ffn", "xema_op_gated_ffn_grad", "xema_op_lora", "xema_lora_work_bytes", "xema_strerror",
+    "xema_op_rmsnorm_rope", "xema_op_gemm", "xema_gemm_tile", "xema_op_gemm_in_tile", "xema_op_attention", "xema_op_rms_norm", "xema_op_gated_ffn", "xema_op_gated_ffn_grad", "xema_op_lora", "xema_lora_work_bytes", "xema_op_gated_ffn_in", "xema_op_gated_ffn_grad_in", "xema_op_lora_in", "xema_strerror",
     "xema_last_cuda_error", "xema_version", "xema_selftest_wait_timeout",
     "xema_pluggable_malloc", "xema_pluggable_free", "xema_pluggable_mode", "xema_pluggable_recorded",
     "xema_pluggable_set_plan", "xema_pluggable_step_begin", "xema_pluggable_stats",
@@ -111,6 +112,10 @@ class xema_lora_args(C.Structure):
                 ("rank", C.c_int32), ("n_adapters", C.c_int32)]
 
 
+class xema_ff_shape(C.Structure):
+    _fields_ = [("kernel", C.c_int32), ("pair", C.c_int32), ("columns", C.c_int32), ("share", C.c_int32), ("features", C.c_int32)]
+
+
 _lib = None
 
 
@@ -177,6 +182,9 @@ def lib() -> C.CDLL:
             "xema_op_gated_ffn_grad": [P(xema_gated_ffn_grad_args), vp, vp],
             "xema_op_lora": [P(xema_lora_args), vp, vp],
             "xema_lora_work_bytes": [i32, i32, i32],
+            "xema_op_gated_ffn_in": [P(xema_gated_ffn_args), P(xema_ff_shape), vp, vp],
+            "xema_op_gated_ffn_grad_in": [P(xema_gated_ffn_grad_args), P(xema_ff_shape), P(xema_ff_shape), vp, vp],
+            "xema_op_lora_in": [P(xema_lora_args), P(xema_ff_shape), i32, vp, vp],
             "xema_last_cuda_error": [],
             "xema_selftest_wait_timeout": [vp, i64, vp, vp],
         }
@@ -614,3 +622,15 @@ def xema_op_lora(args: xema_lora_args, status=None, stream=0):
 
 def xema_lora_work_bytes(batch: int, rows: int, rank: int) -> int:
     return lib().xema_lora_work_bytes(batch, rows, rank)
+
+
+def xema_op_gated_ffn_in(args: xema_gated_ffn_args, shape: xema_ff_shape, status=None, stream=0):
+    _check(lib().xema_op_gated_ffn_in(C.byref(args), C.byref(shape), status, stream), "xema_op_gated_ffn_in")
+
+
+def xema_op_gated_ffn_grad_in(args: xema_gated_ffn_grad_args, dx: xema_ff_shape, dw: xema_ff_shape, status=None, stream=0):
+    _check(lib().xema_op_gated_ffn_grad_in(C.byref(args), C.byref(dx), C.byref(dw), status, stream), "xema_op_gated_ffn_grad_in")
+
+
+def xema_op_lora_in(args: xema_lora_args, shape: xema_ff_shape, share_t=0, status=None, stream=0):
+    _check(lib().xema_op_lora_in(C.byref(args), C.byref(shape), share_t, status, stream), "xema_op_lora_in")

@@ -8,6 +8,9 @@ namespace {
 // Rows up to which the kernels for few tokens are considered.
 constexpr int kFewRows = 1024;
 
+// Whether a product of so many rows can run in the kernel that is asked for.
+bool can_run(const xema_ff_shape* in, int rows, bool gated) { return !in || is_tile(*in, gated) || (in->kernel == XEMA_FF_FEW && rows <= kFewRows); }
+
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // dg = dh * zu * act'(zg), du = dh * act(zg), eight neighbouring features a thread.  `d` may be `z`: a thread reads what it overwrites.
@@ -47,7 +50,7 @@ __global__ void __launch_bounds__(256) gated_grad_kernel(const __nv_bfloat16* dh
 }
 }  // namespace
 
-int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStream_t stream) {
+int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* in) {
   const int unit = a.is_e4m3 ? 16 : 8, elem = a.is_e4m3 ? 1 : 2;
   if (a.rows < 0 || a.width < unit || a.width % unit || a.ffn < 8 || a.ffn % 8) return XEMA_EINVAL;
   if (a.rows > kMaxSize || a.width > kMaxSize || a.ffn > kMaxSize) return XEMA_EINVAL;
@@ -80,8 +83,9 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
   p.up_scale = a.up_scale;
   p.status = status;
   p.off_line = ((a.rows > 1 ? a.ldx : 0) | a.ldw) * elem % 128 != 0;
-  const Shape shape = pick_shape(p, p.k_main, true);
-  if (a.rows <= kFewRows) {
+  if (!can_run(in, a.rows, true)) return XEMA_EINVAL;
+  const Shape shape = take_shape(p, p.k_main, true, in);
+  if (a.rows <= kFewRows && (!in || in->kernel == XEMA_FF_FEW)) {
     skinny::Params q = {};
     q.rows = a.rows;
     q.cols = a.ffn;
@@ -95,9 +99,10 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
     q.z = static_cast<__nv_bfloat16*>(a.z);
     q.status = status;
     long long ns = 0;
-    int rc = a.is_e4m3 ? skinny::plan<skinny::Kind::kGated, true>(&q, &ns) : skinny::plan<skinny::Kind::kGated, false>(&q, &ns);
+    const int s = in ? in->share : 0, r = in ? in->features : 0;
+    int rc = a.is_e4m3 ? skinny::plan<skinny::Kind::kGated, true>(&q, &ns, s, r) : skinny::plan<skinny::Kind::kGated, false>(&q, &ns, s, r);
     if (rc) return rc;
-    if (ns < shape_ns(p, shape, p.k_main, true)) {
+    if (in || ns < shape_ns(p, shape, p.k_main, true)) {
       skinny::Maps m = {};
       rc = encode_tmap_tile(&m.a, a.w_gate, elem, a.width, a.ffn, 1, a.ldw, 0, step, q.R);
       if (!rc) rc = encode_tmap_tile(&m.a2, a.w_up, elem, a.width, a.ffn, 1, a.ldw, 0, step, q.R);
@@ -116,7 +121,8 @@ int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStr
   return a.is_e4m3 ? launch<Form::kGated, true>(m, p, shape, stream) : launch<Form::kGated, false>(m, p, shape, stream);
 }
 
-int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* status, cudaStream_t stream) {
+int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* dx_in,
+                          const xema_ff_shape* dw_in) {
   if (a.rows < 0 || a.width < 8 || a.width % 8 || a.ffn < 8 || a.ffn % 8) return XEMA_EINVAL;
   if (a.rows > kMaxSize || a.width > kMaxSize || a.ffn > kMaxSize) return XEMA_EINVAL;
   if (a.activation != XEMA_ACT_SILU && a.activation != XEMA_ACT_GELU_TANH) return XEMA_EINVAL;
@@ -142,6 +148,8 @@ int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* statu
   if (want_w && !on16(a.x)) return XEMA_EALIGN;
   if (want_x && (!on16(a.w_gate) || !on16(a.w_up) || !on16(a.dx) || a.ldw % 8)) return XEMA_EALIGN;
   if (a.rows > 1 && (a.lddh % 8 || (want_w && a.ldx % 8) || (want_x && a.lddx % 8))) return XEMA_EALIGN;
+
+  if (!can_run(dx_in, a.rows, false) || (dw_in && !is_tile(*dw_in, false))) return XEMA_EINVAL;
 
   const long long row = 2LL * a.width, z_bytes = 2LL * a.rows * a.ffn;
   const Rows in[] = {{a.dh, a.rows, 2LL * a.ffn, a.lddh * 2}, {want_w ? a.x : nullptr, a.rows, row, a.ldx * 2},
@@ -169,10 +177,10 @@ int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* statu
     p.k_main = (a.ffn + 63) / 64;
     p.status = status;
     p.off_line = (a.ffn | a.ldw) * 2 % 128 != 0;
-    const Shape shape = pick_shape(p, 2 * p.k_main, false);
+    const Shape shape = take_shape(p, 2 * p.k_main, false, dx_in);
     skinny::Params q = {};
     long long ns = 0;
-    if (a.rows <= kFewRows) {
+    if (a.rows <= kFewRows && (!dx_in || dx_in->kernel == XEMA_FF_FEW)) {
       q.rows = a.rows;
       q.cols = a.width;
       q.k_blocks = 2 * p.k_main;
@@ -180,9 +188,9 @@ int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* statu
       q.out = static_cast<__nv_bfloat16*>(a.dx);
       q.ldo = a.rows > 1 ? a.lddx : a.width;
       q.status = status;
-      rc = skinny::plan<skinny::Kind::kGradX, false>(&q, &ns);
+      rc = skinny::plan<skinny::Kind::kGradX, false>(&q, &ns, dx_in ? dx_in->share : 0, dx_in ? dx_in->features : 0);
     }
-    if (!rc && ns && ns < shape_ns(p, shape, 2 * p.k_main, false)) {
+    if (!rc && ns && (dx_in || ns < shape_ns(p, shape, 2 * p.k_main, false))) {
       skinny::Maps m = {};
       rc = encode_tmap_tile(&m.a, a.w_gate, 2, a.width, a.ffn, 1, a.ldw, 0, 64, 64);
       if (!rc) rc = encode_tmap_tile(&m.a2, a.w_up, 2, a.width, a.ffn, 1, a.ldw, 0, 64, 64);
@@ -210,7 +218,7 @@ int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* statu
     if (!rc) rc = encode_tmap_tile(&m.b, a.x, 2, a.width, a.rows, 1, a.ldx, 0, 64, 64);
     if (!rc) rc = encode_tmap_tile(&m.out, a.dw_gate, 2, a.width, a.ffn, 1, a.lddw, 0, 32, 32);
     if (!rc) rc = encode_tmap_tile(&m.out2, a.dw_up, 2, a.width, a.ffn, 1, a.lddw, 0, 32, 32);
-    if (!rc) rc = launch<Form::kGradW, false>(m, p, pick_shape(p, p.k_main, false), stream);
+    if (!rc) rc = launch<Form::kGradW, false>(m, p, take_shape(p, p.k_main, false, dw_in), stream);
   }
   return rc;
 }

@@ -185,9 +185,11 @@ bool rows_meet(const Rows& a, const Rows& b);
 
 // ---- gated feed-forward, adapters, RMSNorm: arguments as in xema.h, checked here --------------
 int launch_rms_norm(const xema_rms_norm_args& a, cudaStream_t stream);
-int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStream_t stream);
-int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* status, cudaStream_t stream);
-int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stream);
+// (shapes: null for those that are estimated to be fastest)
+int launch_gated_ffn(const xema_gated_ffn_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* in = nullptr);
+int launch_gated_ffn_grad(const xema_gated_ffn_grad_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* dx_in = nullptr,
+                          const xema_ff_shape* dw_in = nullptr);
+int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* in = nullptr, int share_t = 0);
 unsigned long long lora_work_bytes(int batch, int rows, int rank);
 
 }  // namespace xema

@@ -117,7 +117,7 @@ unsigned long long lora_work_bytes(int batch, int rows, int rank) {
   return 2ull * batch * rows * rank;
 }
 
-int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stream) {
+int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stream, const xema_ff_shape* in, int share_t) {
   if (a.batch < 0 || a.rows < 0 || a.K < 8 || a.K % 8 || a.N < 8 || a.N % 8 || a.n_adapters < 0) return XEMA_EINVAL;
   if (a.batch > kMaxSize || a.rows > kMaxSize || a.K > kMaxSize || a.N > kMaxSize) return XEMA_EINVAL;
   if (a.rank < 8 || a.rank % 8 || a.rank > XEMA_LORA_MAX_RANK) return XEMA_EINVAL;
@@ -134,10 +134,10 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   if (reinterpret_cast<uintptr_t>(a.bias) & 1) return XEMA_EALIGN;
   const Batches x = {{a.x, a.rows, a.K * 2LL, a.ldx * 2}, a.batch, a.x_batch_rows}, out = {{a.out, a.rows, a.N * 2LL, a.ldo * 2}, a.batch, a.out_batch_rows};
   const Rows work = {a.n_adapters > 0 ? a.work : nullptr, 1, (long long)lora_work_bytes(a.batch, a.rows, a.rank), 0};
-  const Rows in[] = {{a.w, a.N, a.K * 2LL, a.ldw * 2}, {a.lora_a, 1, 2LL * a.n_adapters * a.rank * a.K, 0},
+  const Rows operands[] = {{a.w, a.N, a.K * 2LL, a.ldw * 2}, {a.lora_a, 1, 2LL * a.n_adapters * a.rank * a.K, 0},
                      {a.lora_b, 1, 2LL * a.n_adapters * a.rank * a.N, 0}, {a.bias, 1, 2LL * a.N, 0}, {a.adapter, 1, 4LL * a.batch, 0},
                      {a.n_adapters > 0 ? a.scale : nullptr, 1, 4LL * a.n_adapters, 0}};
-  for (const Rows& i : in)
+  for (const Rows& i : operands)
     if (rows_meet(out.all(), i) || rows_meet(work, i)) return XEMA_EINVAL;
   if (rows_meet(out.all(), work) || rows_meet(x.all(), work) || batches_meet(x, out)) return XEMA_EINVAL;
   Params p = {};
@@ -152,7 +152,10 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   p.behind = a.n_adapters > 0;
   p.status = status;
   p.off_line = ((total > 1 ? a.ldx : 0) | a.ldw) * 2 % 128 != 0;
-  const Shape shape = pick_shape(p, p.k_main + p.k_more, false);
+  if (in && !is_tile(*in, false) && !(in->kernel == XEMA_FF_FEW && a.rows <= kFewRows) &&
+      !(in->kernel == XEMA_FF_SINGLE && a.rows == 1 && total <= kFewTokens))
+    return XEMA_EINVAL;
+  const Shape shape = take_shape(p, p.k_main + p.k_more, false, in);
   const long long shared_ns = shape_ns(p, shape, p.k_main + p.k_more, false);
 
   // The kernels for few tokens: single tokens, or a few rows a request.  (Which of them does not depend on strides.)
@@ -174,14 +177,15 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   q.status = status;
   skinny::Params q1 = q;
   int rc = XEMA_OK;
-  if (a.rows <= kFewRows) {
+  const int only_s = in ? in->share : 0, only_r = in ? in->features : 0;
+  if (a.rows <= kFewRows && (!in || in->kernel == XEMA_FF_FEW)) {
     q.rows = a.rows;
     q.batch = a.batch;
-    if ((rc = skinny::plan<Kind::kPacked, false>(&q, &ns))) return rc;
+    if ((rc = skinny::plan<Kind::kPacked, false>(&q, &ns, only_s, only_r))) return rc;
   }
-  if (a.rows == 1 && total <= kFewTokens) {
+  if (a.rows == 1 && total <= kFewTokens && (!in || in->kernel == XEMA_FF_SINGLE)) {
     q1.rows = (int)total;
-    if ((rc = skinny::plan<Kind::kLora, false>(&q1, &ns1))) return rc;
+    if ((rc = skinny::plan<Kind::kLora, false>(&q1, &ns1, only_s, only_r))) return rc;
     ns1 += total * a.N * a.rank / 3000;        // t B^T beside the products
   }
   // t: by the CUDA cores beside a projection of either kind, or by a launch that takes SMs of its own
@@ -204,12 +208,12 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
       bool beside = false;
       long long t_ns = 0;
       if ((rc = skinny::tile_tokens<Kind::kShrink>(&s[i]))) return rc;
-      const int split = shrink_split(s[i], i ? (long long)q.f_tiles * q.tiles * q.S : tile_count(p, shape, false), i ? false : shape.pair, &beside);
+      const int split = share_t ? share_t : shrink_split(s[i], i ? (long long)q.f_tiles * q.tiles * q.S : tile_count(p, shape, false), i ? false : shape.pair, &beside);
       if ((rc = skinny::plan<Kind::kShrink, false>(&s[i], &t_ns, split))) return rc;
       if (!beside) (i ? packed_ns : tiled_ns) += t_ns;
     }
   }
-  const bool packed = ns && packed_ns < tiled_ns && (!ns1 || packed_ns < ns1), flat = !packed && ns1 && ns1 < tiled_ns;
+  const bool packed = ns && (in || (packed_ns < tiled_ns && (!ns1 || packed_ns < ns1))), flat = !packed && ns1 && (in || ns1 < tiled_ns);
 
   if (a.n_adapters > 0) {
     if (flat || tokens_alone) {

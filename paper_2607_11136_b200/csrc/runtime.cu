@@ -1175,6 +1175,21 @@ int xema_op_lora(const xema_lora_args* a, void* status_dev, void* stream) {
   return launch_lora(*a, static_cast<unsigned int*>(status_dev), reinterpret_cast<cudaStream_t>(stream));
 }
 
+int xema_op_gated_ffn_in(const xema_gated_ffn_args* a, const xema_ff_shape* in, void* status_dev, void* stream) {
+  if (!a || !in) return XEMA_EINVAL;
+  return launch_gated_ffn(*a, static_cast<unsigned int*>(status_dev), reinterpret_cast<cudaStream_t>(stream), in);
+}
+
+int xema_op_gated_ffn_grad_in(const xema_gated_ffn_grad_args* a, const xema_ff_shape* dx, const xema_ff_shape* dw, void* status_dev, void* stream) {
+  if (!a || !dx || !dw) return XEMA_EINVAL;
+  return launch_gated_ffn_grad(*a, static_cast<unsigned int*>(status_dev), reinterpret_cast<cudaStream_t>(stream), dx, dw);
+}
+
+int xema_op_lora_in(const xema_lora_args* a, const xema_ff_shape* in, int32_t share_t, void* status_dev, void* stream) {
+  if (!a || !in) return XEMA_EINVAL;
+  return launch_lora(*a, static_cast<unsigned int*>(status_dev), reinterpret_cast<cudaStream_t>(stream), in, share_t);
+}
+
 uint64_t xema_lora_work_bytes(int32_t batch, int32_t rows, int32_t rank) { return lora_work_bytes(batch, rows, rank); }
 
 int xema_last_cuda_error(void) { return t_last_cuda_error; }

@@ -498,10 +498,11 @@ inline int tile_tokens(Params* p) {
 
 // Fills S, R, split and what follows from them: the pair with the shortest estimate, in clocks, of what bounds a CTA -- its MMAs (26
 // clocks + operand bytes / 170 each, and the round of a stage's barriers), its fill (57 bytes a clock) or its share of the memory's
-// rate (3400 bytes a clock for all).  *ns: the estimate.  only_s: this S and no other.
+// rate (3400 bytes a clock for all).  *ns: the estimate.  only_s, only_r: this S or R and no other.
 template <Kind KIND, bool F8>
-int plan(Params* p, long long* ns, int only_s = 0) {
+int plan(Params* p, long long* ns, int only_s = 0, int only_r = 0) {
   constexpr bool GATED = KIND == Kind::kGated, PACKED = KIND == Kind::kPacked;
+  if (only_r < 0 || only_r > 128 || only_r % (KIND == Kind::kGradX ? 64 : 8)) return XEMA_EINVAL;
   if (int rc = tile_tokens<KIND>(p)) return rc;
   const int nt = p->nt, groups = p->cols / 8, token_tiles = p->tiles;
   const long long mma = 26 + (4096 + nt * 32) / 170;
@@ -522,6 +523,7 @@ int plan(Params* p, long long* ns, int only_s = 0) {
       const int waves = waves0 + choice / 2, per_sm = 1 + choice % 2;
       const long long fit = (units + (long long)clusters * waves - 1) / ((long long)clusters * waves);
       q.R = choice >= 4 ? 128 : (int)std::min<long long>(128, 8 * fit);
+      if (only_r) q.R = only_r;
       if (KIND == Kind::kGradX) q.R = q.R > 64 ? 128 : 64;
       if (KIND == Kind::kShrink) q.R = p->cols;
       q.split = GATED && q.R > 64;

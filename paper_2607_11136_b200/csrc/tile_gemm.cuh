@@ -501,6 +501,14 @@ inline Shape pick_shape(const Params& p, long long steps, bool gated) {
     if (shape_ns(p, {1, bn}, steps, gated) < shape_ns(p, best, steps, gated)) best = {1, bn};
   return best;
 }
+// That one, or the one that a caller asks for, and whether there is such a one.
+inline Shape take_shape(const Params& p, long long steps, bool gated, const xema_ff_shape* in) {
+  return in && in->kernel == XEMA_FF_TILES ? Shape{in->pair != 0, in->columns} : pick_shape(p, steps, gated);
+}
+inline bool is_tile(const xema_ff_shape& in, bool gated) {
+  const int bn = in.columns;
+  return in.kernel == XEMA_FF_TILES && (in.pair ? bn >= 128 && bn <= 256 && bn % (gated ? 64 : 32) == 0 : bn == 128);
+}
 // Rows of B that one load brings: of one of two halves where a tile has two (gated), or a CTA's share.
 inline int b_box(const Shape& s, bool gated) { return s.pair || gated ? s.bn / 2 : s.bn; }
 
