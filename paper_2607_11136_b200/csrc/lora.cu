@@ -158,7 +158,8 @@ int launch_lora(const xema_lora_args& a, unsigned int* status, cudaStream_t stre
   const Shape shape = take_shape(p, p.k_main + p.k_more, false, in);
   const long long shared_ns = shape_ns(p, shape, p.k_main + p.k_more, false);
 
-  // The kernels for few tokens: single tokens, or a few rows a request.  (Which of them does not depend on strides.)
+  // The kernels for few tokens: single tokens, or a few rows a request.  (Strides count in the choice where they take rows off the 128-byte lines,
+  // through the estimate for tiles; results then differ in their last bits.)
   using skinny::Kind;
   skinny::Params q = {};
   long long ns = 0, ns1 = 0;
