@@ -46,6 +46,7 @@ const Tensor& tensor(PyObject* o, const char* name, at::ScalarType type, int64_t
   if (t.scalar_type() != type) refuse(std::string(name) + ": want " + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
   if (t.dim() != rank) refuse(std::string(name) + ": want " + std::to_string(rank) + " dimensions");
   if (rank > 0 && t.size(rank - 1) > 1 && t.stride(rank - 1) != 1) refuse(std::string(name) + ": the last dimension has to be contiguous");
+  if (t.numel() > 0 && (!t.has_storage() || !t.storage().data())) refuse(std::string(name) + ": a tensor of this kind has no memory");
   return t;
 }
 void sized(const Tensor& t, const char* name, at::IntArrayRef want) {
