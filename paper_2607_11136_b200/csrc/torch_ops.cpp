@@ -3,10 +3,12 @@
 // small call's time is the host's: the same steps in Python take 9 to 14 us beside a kernel of 2 to 5.
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <string>
 
@@ -46,6 +48,7 @@ const Tensor& tensor(PyObject* o, const char* name, at::ScalarType type, int64_t
   if (t.scalar_type() != type) refuse(std::string(name) + ": want " + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
   if (t.dim() != rank) refuse(std::string(name) + ": want " + std::to_string(rank) + " dimensions");
   if (rank > 0 && t.size(rank - 1) > 1 && t.stride(rank - 1) != 1) refuse(std::string(name) + ": the last dimension has to be contiguous");
+  if (t._fw_grad(0).defined()) refuse(std::string(name) + ": carries a forward-mode derivative, which the result would not carry on");
   if (t.numel() > 0 && (!t.has_storage() || !t.storage().data())) refuse(std::string(name) + ": a tensor of this kind has no memory");
   return t;
 }
@@ -78,8 +81,11 @@ PyObject* answer(int rc, const Tensor (&t)[N]) {
   for (int i = 0; out && i < N; ++i) PyTuple_SET_ITEM(out, i, wrap(t[i]));
   return out;
 }
+// At the head of each operator.
 void argc(Py_ssize_t n, Py_ssize_t want) {
   if (n != want) refuse("wrong number of arguments");
+  if (torch::jit::tracer::isTracing() || c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value())
+    refuse("this operator cannot be traced: the traced program would hold the result of this call");
 }
 bool truth(PyObject* o) {
   const int v = PyObject_IsTrue(o);

@@ -11,7 +11,8 @@ the operators do not take raise ValueError or XemaError before anything is launc
 index beyond the adapters, a wait that ran out) is raised by `check`.
 
 The functions are not recorded by autograd: while gradients are on, operands that require one are refused.  In a training program they stand in a
-torch.autograd.Function, or under torch.no_grad(), and gated_ffn_backward is the gradient of gated_ffn.
+torch.autograd.Function, or under torch.no_grad(), and gated_ffn_backward is the gradient of gated_ffn.  Forward-mode derivatives, vmap and tracers
+(torch.jit.trace, make_fx) are refused; torch.compile runs its graphs around the calls.
 """
 from __future__ import annotations
 
