@@ -1,8 +1,8 @@
 // A projection that all requests of a batch share, beside each request's own low-rank adapter:
 //   y[b] = x[b] W^T + bias + t[b] B_a^T,  t[b] = scale_a (x[b] A_a^T),  a = adapter[b].
 // Two launches: t, and the projection.  With many tokens the projection's accumulator takes t B^T as further steps along K; with
-// few it streams W, and t B^T is worked out beside it.  us, back to back in a graph: 4 x 4608 tokens of 4096 x 4096, rank 64, 425 (t alone 30);
-// 60 x 30 tokens of 1024 x 2048 20 (32 with a tile of 128 rows a request); 256 single tokens of 4096 x 4096 30 (176 with 16 columns each).
+// few it streams W, and t B^T is worked out beside it.  us, back to back in a graph: 4 x 4608 tokens of 4096 x 4096, rank 64, 426 (t alone 30);
+// 60 x 30 tokens of 1024 x 2048 18 (30 with a tile of 128 rows a request); 256 single tokens of 4096 x 4096 26 (204 with 16 columns each).
 #include "skinny_gemm.cuh"
 
 namespace xema {
@@ -90,8 +90,9 @@ bool batches_meet(const Batches& a, const Batches& b) {
 // CTAs that share K of t, for a projection of `tiles` CTAs or (pair) pairs.  The projection starts on the SMs that t leaves free (a pair needs
 // both SMs of two neighbours) and has its first waves to go before it needs t: one CTA a tile where the projection fills the device for longer
 // than a wave, else as many as there is room for beside it, and (with enough of K to share) four where there is none and everything waits for
-// t.  us with 1 / 2 / 4: 5 x 397 tokens 1544 x 2312 27.0 / 28.0 / 32.1, 3 x 1000 4096 x 2048 39.4 / 46.0 / 44.0; 2 x 100 4096 x 4096 21.4 / 18.0 /
-// 18.0, 1 x 333 2048 x 2048 14.9 / 12.9 / 12.2; 7 x 300 3000 x 1024 40.7 / 36.9 / 34.5; 1 x 2000 1024 x 1024 12.4 / 14.4 / 14.2.
+// t.  us with 1 / 2 / 4, rank 16: pairs of 192 columns 5 x 397 tokens 1544 x 2312 26.5 / 27.8 / 31.8, 3 x 1000 4096 x 2048 39.0 / 45.1 / 43.7; 128 x
+// 128 2 x 100 4096 x 4096 20.4 / 20.3 / 20.1, 1 x 333 2048 x 2048 13.9 / 11.5 / 10.9, 1 x 2000 1024 x 1024 11.2 / 13.6 / 13.4.  Where it picks worse:
+// 7 x 300 3000 x 1024, pairs of 256, 25.1 / 31.7 / 31.6.
 // *beside: whether t runs beside the projection's first tiles and takes no time of its own.
 int shrink_split(const skinny::Params& s, long long tiles, bool pair, bool* beside) {
   const long long slots = pair ? sm_count() / 2 : sm_count(), left = slots - tiles;

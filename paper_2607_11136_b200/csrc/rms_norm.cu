@@ -125,7 +125,7 @@ __device__ __forceinline__ float quotient(float v, float scale, float inv) {
 // A block per row, or (WARP) a warp of eight, the row in registers: every byte is read and written once.  Thread t holds the groups of E
 // values t, t + T, ...  (T threads, V groups); E is what the strides and addresses allow to be moved at once.
 // Bound by HBM: 16384 x 4096, residual in bf16, result in e4m3, 70 us (6.7 TB/s; 73 with 16 values a thread, 85 with 8), 8192 x 8192 in
-// bf16 79 us (6.8), one row 2.3 us.  Streaming stores change nothing, loads past the L1 lose 9 %.
+// bf16 79 us (6.8), one row 2.2 us.  Streaming stores change nothing, loads past the L1 lose 9 %.
 template <typename R, typename Out, int E, int V, bool WARP>
 __global__ void __launch_bounds__(WARP || E * V <= 8 ? 256 : E * V <= 32 ? 512 : 1024) rms_norm_kernel(const xema_rms_norm_args p) {
   __shared__ float s_sum[32], s_max[32];
@@ -231,7 +231,8 @@ int launch(const xema_rms_norm_args& a, cudaStream_t st) {
 }
 
 // Rows whose values lie on no common boundary (an odd width or stride): the row goes through shared memory, so that all but its ends
-// moves 16 bytes at a time, with all of a row's loads under way together.  9000 x 2299, result in e4m3: 168 us one value after the other.
+// moves 16 bytes at a time, with all of a row's loads under way together.  9000 x 2299, result in e4m3: 54 us (2.7 TB/s; 168 one value after the other).  Bound by the accesses
+// to shared memory, two or three a value and two bytes each, and by the gain, which comes value by value for each row.
 constexpr int kOddValues = 16, kOddMaxD = 8192;       // values of a thread
 template <typename T>
 struct RowLoad {

@@ -14,9 +14,9 @@
 //            adapter's second product is an MMA on the columns of its request alone -- no other request's sums meet its values
 //
 // Bound by HBM where the weights come from there: gated, one token of 4096 x 11264 in bf16 (185 MB) 31.4 us (5.9 TB/s), 24 tokens of 4096 x
-// 16384 in e4m3 (135 MB) 23.6 us (5.7 TB/s), back to back in a graph; with 128 x 128 tiles 52 and 36.  4096 x 4096 by one CTA of 32
-// features each 14.1 us and 20.6 with a single block a stage; K shared by 2 or 4 CTAs 13.7.  dx of 333 tokens, 512 x 8192: 54 us by single CTAs,
-// 23 with K shared by 4.  48 tokens with adapters of rank 16, 4096 x 4096: 145 us by tiles of a request each, 12.6 here.
+// 16384 in e4m3 (135 MB) 23.4 us (5.8 TB/s), back to back in a graph; with 128 x 128 tiles 52 and 36.  4096 x 4096 by one CTA of 32
+// features each 13.7 us (once 20.6, with a single block a stage); K shared by 2 or 4 CTAs 14.0 and 13.7.  dx of 333 tokens, 512 x 8192, with dg and
+// du: 57 us by single CTAs, 25 with K shared by 4.  48 tokens with adapters of rank 16, 4096 x 4096: 141 us by tiles of a request each, 12.3 here.
 #pragma once
 #include "tile_gemm.cuh"
 

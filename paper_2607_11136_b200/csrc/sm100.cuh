@@ -1,5 +1,5 @@
 // Thin inline-PTX layer for sm_100a: mbarrier, TMA (cp.async.bulk.tensor), tcgen05 MMA with
-// TMEM accumulators, and the descriptor encodings they take.  Every wait is bounded.
+// TMEM accumulators, and the descriptor encodings they take.  Every wait on an mbarrier is bounded.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>

@@ -15,11 +15,13 @@
 //   warps 2-9 epilogue of the finished accumulator (thread = row, two warps a row take 32 columns in turn) while the next tile's products
 //             fill the other one
 // Barriers and ends of the pair form are those of the block's GEMM: all loads of a pair complete on the even CTA's full[], releases
-// are multicast commits, every wait is bounded, and no CTA leaves while its peer may still touch it.
+// are multicast commits, every wait on an mbarrier is bounded and reported where it gives up, and no CTA leaves while its peer may still
+// touch it.  griddepcontrol.wait, the TMEM allocation, __syncthreads and the cluster barriers have no limit, and a launch that stood in one of them
+// would leave no status: they wait for earlier launches, which hold nothing of this one, and for warps whose own waits end.
 //
-// Bound by the tensor pipe and, in long runs, by the board's power: single launches of 8192 x 4096 x 11264 gated 941 us (1606 TFLOP/s), its dx 935
-// (1617) and dW 974 (1552; 19.03 waves of tiles), 8192 x 4096 x 12288 gated in e4m3 513 us (3.2 PFLOP/s), 4 x 4608 x 4096 x 4096 with adapters
-// of rank 64 380 us (1640).  Eight epilogue warps against four: 5 to 12 % faster where the reduction is short, no difference where it is long.
+// Bound by the tensor pipe and, in long runs, by the board's power: launches by themselves of 8192 x 4096 x 11264 gated 926 to 937 us (1614 to
+// 1633 TFLOP/s; 963 with z), its dx 948 (1595) and dW 974 (1552; 19.03 waves of tiles), 8192 x 4096 x 12288 gated in e4m3 525 us (3.1 PFLOP/s),
+// 4 x 4608 x 4096 x 4096 with adapters of rank 64 386 us (1630).  Eight epilogue warps against four: 5 to 12 % faster where the reduction is short, no difference where it is long.
 #pragma once
 #include <algorithm>
 
@@ -113,8 +115,8 @@ __device__ __forceinline__ float act_q(float z, int act) {
 __device__ __forceinline__ float sigmoid_f(float q) { return __fdividef(1.f, 1.f + __expf(-q)); }
 
 // What the gradient is given of zg and zu: both in bf16, and in a third plane what that leaves out, a signed byte each in steps of 2^-15 of
-// the value's power of two (zg in the low one).  zg and zu in bf16 alone would double the square of the gradients' error: relative to
-// the norm 3.1e-3 against 2.4e-3, of which 2.4e-3 are the roundings of dg, du and the results.
+// the value's power of two (zg in the low one).  zg and zu in bf16 alone would nearly double the square of the gradients' error: relative
+// to the norm 3.1e-3 against 2.35e-3, which is what the roundings of dg and du and of the results leave.
 __device__ __forceinline__ int low_byte(float z) {
   const float h = __bfloat162float(__float2bfloat16_rn(z));
   const uint32_t e = __float_as_uint(h) & 0x7f800000u;
@@ -522,7 +524,8 @@ int launch(const Maps& maps, Params p, const Shape& shape, cudaStream_t stream) 
   p.b_bytes = (FORM == Form::kGradX || FORM == Form::kGradW ? (b_rows + 63) / 64 * 64 : b_rows) * kStepBytes;
   p.stages = std::min(kMaxStages, kStageArea / (ksub * (kOperandBytes + p.b_bytes)));
   // The gradients' products start when everything before them has ended: chained to each other and to the kernel that makes dg and du,
-  // a backward pass in a graph stopped for good in some ten thousands of passes, for a reason that was not found.
+  // a backward pass in a graph stopped for good in some ten thousands of passes, for a reason that was not found.  (Instructions that
+  // want whole warps followed single lanes' work then, named barriers without a limit among them; the chain has not run since that is mended.)
   constexpr bool CHAINED = FORM != Form::kGradX && FORM != Form::kGradW;
   if (!shape.pair) {
     static PerDeviceInt attr_done;

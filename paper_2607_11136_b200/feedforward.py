@@ -6,7 +6,9 @@ feed-forward with its gradients, and a projection with the adapters of many requ
     y = lora_linear(h, w_down, lora_a, lora_b, lora_scale, adapter)
 
 Everything runs on the current stream of the tensors' device, without synchronising; results and workspaces come from
-torch's allocator unless the caller gives the results.  Last dimensions are contiguous, other strides are free.  Arguments that
+torch's allocator unless the caller gives the results.  Last dimensions are contiguous.  Between rows rms_norm takes any
+stride; the products want rows on 16-byte boundaries (strides of 8 values, e4m3: 16) that do not lie over one another, so a dh that was expanded
+from a scalar has to be made contiguous.  Arguments that
 the operators do not take raise ValueError or XemaError before anything is launched; what a kernel finds out later (an adapter
 index beyond the adapters, a wait that ran out) is raised by `check`.
 
